@@ -68,6 +68,7 @@ struct MxParams {
   __nv_bfloat16* y;                        // phase 2: y_perm [rows, d]
   uint8_t* h_scale;                        // tiled scales of H
   int h_kblocks;                           // its k-blocks per row block (those of the widest group)
+  bool sector;                             // rows of this phase's output begin on 32-byte boundaries
   const int32_t* counts;                   // rows of an expert's segment that hold tokens
   const int32_t* aligned;
   const int32_t* tile_count;
@@ -101,7 +102,8 @@ __device__ __forceinline__ void umma_mx8(uint32_t d_tmem, uint64_t adesc, uint64
         ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
 }
 
-// 32 bytes of a row, the first `valid` (a multiple of 8) of which exist; sector: the address is a multiple of 32
+// 32 bytes of a row, the first `valid` (a multiple of 8) of which exist; sector: the address is a multiple of
+// 32, which takes the buffer's own address as well as the row's length (callers promise 16-byte alignment only)
 __device__ __forceinline__ void store_sector(uint8_t* p, bool sector, int valid, const uint32_t (&o)[8]) {
   if (sector && valid >= 32) {
     asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
@@ -341,7 +343,7 @@ __global__ void __launch_bounds__(kThreadsMx, 1) mx8_grouped_kernel(const __grid
             o[j] = mx8_pack4(lo.x, lo.y, hi.x, hi.y);
           }
           const int col = t.n0 + 32 * c;
-          if (rows_ok) store_sector(p.h + row * p.h_pitch + col, (p.h_pitch & 31) == 0, W - col, o);
+          if (rows_ok) store_sector(p.h + row * p.h_pitch + col, p.sector, W - col, o);
         }
         if (rows_ok)
           *reinterpret_cast<uint32_t*>(p.h_scale + ((int64_t)(row0 >> 7) * p.h_kblocks + (t.n0 >> 7)) * 512 + lane * 16 + quad * 4) = word;
@@ -368,7 +370,7 @@ __global__ void __launch_bounds__(kThreadsMx, 1) mx8_grouped_kernel(const __grid
               const uint32_t hi = q < 2 ? r0[16 * q + 2 * j + 1] : r1[16 * (q - 2) + 2 * j + 1];
               o[j] = pack2(__uint_as_float(lo), __uint_as_float(hi));
             }
-            store_sector(out + 32 * q, (p.d & 15) == 0, left - 32 * q, o);
+            store_sector(out + 32 * q, p.sector, left - 32 * q, o);
           }
         }
       }
@@ -599,6 +601,7 @@ int32_t launch_experts_mx8(const Dims& D, const void* xp8, const void* xp8_scale
   for (int g = 0; g < D.Ng; ++g) p.W[g] = D.W[g];
   // phase 1
   p.tile_count = tile_count; p.tiles = tiles;
+  p.sector = (((uintptr_t)h8 | hp) & 31) == 0;
   if ((rc = encode_elements(&p.mapA[0], xp8, D.d, dp, rows, 0, BM))) return rc;
   if ((rc = encode_elements(&p.mapA32[0], xp8, D.d, dp, rows, 0, 32))) return rc;
   if ((rc = encode_scales(&p.mapSA, xp8_scale, dkb, rblocks, 0, 1, 0))) return rc;
@@ -611,6 +614,7 @@ int32_t launch_experts_mx8(const Dims& D, const void* xp8, const void* xp8_scale
   if (rc) return rc;
   // phase 2
   p.tile_count = tile_count + 64; p.tiles = tiles + tiles_cap;
+  p.sector = (((uintptr_t)y_perm | (uint64_t)(2 * D.d)) & 31) == 0;
   if ((rc = encode_scales(&p.mapSA, h8_scale, hkb, rblocks, 0, 1, 0))) return rc;
   for (int g = 0; g < D.Ng; ++g) {
     const uint64_t W = D.W[g];
