@@ -7,6 +7,7 @@ library is missing or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
@@ -106,6 +107,22 @@ def exported_symbols() -> List[str]:
 def _check(rc: int, what: str) -> None:
     if rc != 0:
         raise MohgeError("%s failed (%d): %s" % (what, rc, lib().mohge_last_error().decode()))
+
+
+def _require(cond: bool, fmt: str, *args) -> None:
+    if not cond:
+        raise MohgeError(fmt % args)
+
+
+def _require_bytes(what: str, t: torch.Tensor, n: int) -> None:
+    have = t.numel() * t.element_size()
+    _require(have >= n, "%s holds %d bytes, %d are written or read", what, have, n)
+
+
+def _dtype_code(t: torch.Tensor, what: str) -> int:
+    """The library's number of t's type: a type it has no kernels for is refused, never read as another one."""
+    _require(t.dtype in (torch.bfloat16, torch.float32), "%s: %s, expected torch.bfloat16 or torch.float32", what, t.dtype)
+    return BF16 if t.dtype == torch.bfloat16 else F32
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -431,9 +448,13 @@ def mohge_w4_packed_bytes(batch: int, rows: int, K: int, group_size: int) -> int
 
 def mohge_quantize_w4(w, group_size, q, scale):
     """w [.., K] BF16 or FP32 -> q [.., K / 2] uint8, scale [.., ceil(K / group_size)] BF16."""
-    K = w.shape[-1]
-    _check(lib().mohge_quantize_w4(w.numel() // K, K, group_size, BF16 if w.dtype == torch.bfloat16 else F32, _ptr(w),
-                                   _ptr(q), _ptr(scale), _stream()), "mohge_quantize_w4")
+    *lead, K = w.shape
+    code = _dtype_code(w, "mohge_quantize_w4: w")
+    rows = math.prod(lead)
+    _require_bytes("mohge_quantize_w4: q", q, rows * (K // 2))
+    _require_bytes("mohge_quantize_w4: scale", scale, 2 * rows * -(-K // group_size))
+    _check(lib().mohge_quantize_w4(rows, K, group_size, code, _ptr(w), _ptr(q), _ptr(scale), _stream()),
+           "mohge_quantize_w4")
 
 
 def quantize_w4(w, group_size: int):
@@ -495,8 +516,10 @@ def mohge_expert_fwd_w4(cfg, T, x, expert_idx, gate_w, weights: W4Weights, scrat
 def mohge_quantize_mx8(w, q, scale_tiled):
     """w [batch, rows, K] BF16 or FP32 -> operand layout."""
     batch, rows, K = w.shape
-    _check(lib().mohge_quantize_mx8(batch, rows, K, BF16 if w.dtype == torch.bfloat16 else F32, _ptr(w), _ptr(q),
-                                    _ptr(scale_tiled), _stream()), "mohge_quantize_mx8")
+    code = _dtype_code(w, "mohge_quantize_mx8: w")
+    _require_bytes("mohge_quantize_mx8: q", q, batch * rows * mohge_mx8_pitch(K))
+    _require_bytes("mohge_quantize_mx8: scale_tiled", scale_tiled, mohge_mx8_tiled_bytes(batch, rows, K))
+    _check(lib().mohge_quantize_mx8(batch, rows, K, code, _ptr(w), _ptr(q), _ptr(scale_tiled), _stream()), "mohge_quantize_mx8")
 
 
 def quantize_mx8(w):
