@@ -183,6 +183,8 @@ class Config:
         s.dtype = BF16 if self.dtype == "bf16" else F32
         s.alpha_g, s.alpha_e, s.eps = self.alpha_g, self.alpha_e, self.eps
         s.f_norm_by_T, s.fe_mode, s.row_align = self.f_norm_by_T, self.fe_mode, self.row_align
+        # what weights laid out for a layer depend on
+        s.layer = (self.d_model, self.n_groups, self.experts_per_group, tuple(s.group_width[:self.n_groups]))
         self.__dict__["_c_cache"] = (type(self.group_width)(self.group_width), s)
         return s
 
@@ -469,9 +471,36 @@ def quantize_w4(w, group_size: int):
 def mohge_pack_w4(q, scale, group_size, gate_up, packed):
     """q [batch, rows, K / 2] uint8 and its scales -> packed (mohge_w4_packed_bytes bytes)."""
     batch, rows, half = q.shape
-    assert scale.shape == (batch, rows, -(-2 * half // group_size)) and scale.dtype == torch.bfloat16 and q.dtype == torch.uint8
+    _require_form("mohge_pack_w4: q", q, (batch, rows, half), torch.uint8)
+    _require_form("mohge_pack_w4: scale", scale, (batch, rows, -(-2 * half // group_size)), torch.bfloat16)
+    _require_bytes("mohge_pack_w4: packed", packed, mohge_w4_packed_bytes(batch, rows, 2 * half, group_size))
     _check(lib().mohge_pack_w4(batch, rows, 2 * half, group_size, int(gate_up), _ptr(q), _ptr(scale), _ptr(packed),
                                _stream()), "mohge_pack_w4")
+
+
+def _require_form(what: str, t: torch.Tensor, shape, dtype=None) -> None:
+    """shape, and dtype where one is given (1: any type of one byte)."""
+    fits = dtype is None or (t.element_size() == 1 if dtype == 1 else t.dtype == dtype)
+    _require(tuple(t.shape) == tuple(shape) and fits, "%s is %s %s, expected %s %s", what, t.dtype, tuple(t.shape),
+             {None: "any type", 1: "one byte each"}.get(dtype, dtype), tuple(shape))
+
+
+def _require_weights(cfg: Config, what: str, w13, w2, k13=lambda d: d, k2=lambda w: w, dtype=None) -> None:
+    """One w13[g] [N, 2 W_g, k13(d)] and w2[g] [N, d, k2(W_g)] per group of the layer: the library walks as many host
+    pointers, and as many rows and columns behind each, as the config says."""
+    d, Ng, N, W = cfg.c().layer
+    for name, ws, shape in (("w13", w13, lambda w: (N, 2 * w, k13(d))), ("w2", w2, lambda w: (N, d, k2(w)))):
+        _require(len(ws) == Ng, "%s: %d %s for %d groups", what, len(ws), name, Ng)
+        for g in range(Ng):
+            _require_form("%s: %s[%d]" % (what, name, g), ws[g], shape(W[g]), dtype)
+
+
+def _layer_of(cfg: Config, weights) -> mohge_config:
+    """The POD of cfg, which has to be of the layer that `weights` were laid out for."""
+    c = cfg.c()
+    _require(c.layer == weights.layer, "weights of a layer (d, groups, experts per group, widths) = %s with a config of %s",
+             weights.layer, c.layer)
+    return c
 
 
 class W4Weights:
@@ -479,23 +508,26 @@ class W4Weights:
     w2_q[g] [N, d, W_g / 2] with their scales (mohge_quantize_w4's layout)."""
 
     def __init__(self, cfg: Config, group_size: int, w13_q, w13_scale, w2_q, w2_scale):
-        def pack(q, s, shape, gate_up):
-            assert tuple(q.shape) == shape, "%s, expected %s" % (tuple(q.shape), shape)
+        groups = lambda k: -(-k // group_size)  # noqa: E731
+        _require_weights(cfg, "W4Weights: codes", w13_q, w2_q, lambda d: d // 2, lambda w: w // 2, torch.uint8)
+        _require_weights(cfg, "W4Weights: scales", w13_scale, w2_scale, groups, groups, torch.bfloat16)
+
+        def pack(q, s, gate_up):
             out = torch.empty(mohge_w4_packed_bytes(q.shape[0], q.shape[1], 2 * q.shape[2], group_size), dtype=torch.uint8,
                               device=q.device)
             mohge_pack_w4(q, s, group_size, gate_up, out)
             return out
 
-        N, d, W = cfg.experts_per_group, cfg.d_model, list(cfg.group_width)
-        self.group_size = group_size
-        self.w13 = [pack(q, s, (N, 2 * w, d // 2), True) for q, s, w in zip(w13_q, w13_scale, W)]
-        self.w2 = [pack(q, s, (N, d, w // 2), False) for q, s, w in zip(w2_q, w2_scale, W)]
+        self.group_size, self.layer = group_size, cfg.c().layer
+        self.w13 = [pack(q, s, True) for q, s in zip(w13_q, w13_scale)]
+        self.w2 = [pack(q, s, False) for q, s in zip(w2_q, w2_scale)]
         self._a13, self._a2 = _ptr_array(self.w13), _ptr_array(self.w2)
         self.p13, self.p2 = C.cast(self._a13, _P), C.cast(self._a2, _P)
 
     @classmethod
     def quantize(cls, cfg: Config, group_size: int, w13, w2):
         """From the layer's own weights w13[g] [N, 2 W_g, d] and w2[g] [N, d, W_g]."""
+        _require_weights(cfg, "W4Weights.quantize", w13, w2)
         a, b = [quantize_w4(w, group_size) for w in w13], [quantize_w4(w, group_size) for w in w2]
         return cls(cfg, group_size, [x[0] for x in a], [x[1] for x in a], [x[0] for x in b], [x[1] for x in b])
 
@@ -508,7 +540,7 @@ def w4_scratch(cfg: Config, T: int, device="cuda") -> torch.Tensor:
 
 
 def mohge_expert_fwd_w4(cfg, T, x, expert_idx, gate_w, weights: W4Weights, scratch, y, ws, y_add=None):
-    _check(lib().mohge_expert_fwd_w4(C.byref(cfg.c()), T, weights.group_size, _ptr(x), _ptr(expert_idx), _ptr(gate_w),
+    _check(lib().mohge_expert_fwd_w4(C.byref(_layer_of(cfg, weights)), T, weights.group_size, _ptr(x), _ptr(expert_idx), _ptr(gate_w),
                                      weights.p13, weights.p2, _ptr(y_add), _ptr(scratch), _ptr(y), _ptr(ws), _stream()),
            "mohge_expert_fwd_w4")
 
@@ -537,7 +569,7 @@ def mohge_permute_mx8(cfg, T, x8, x8_scale, tok_of_prow, xp8, xp8_scale):
 
 def mohge_expert_fwd_mx8(cfg, T, xp8, xp8_scale, counts, aligned_offsets, weights: "Mx8Weights", h8, h8_scale, y_perm, ws):
     w = weights
-    _check(lib().mohge_expert_fwd_mx8(C.byref(cfg.c()), T, _ptr(xp8), _ptr(xp8_scale), _ptr(counts), _ptr(aligned_offsets),
+    _check(lib().mohge_expert_fwd_mx8(C.byref(_layer_of(cfg, w)), T, _ptr(xp8), _ptr(xp8_scale), _ptr(counts), _ptr(aligned_offsets),
                                       w.p13, w.p13_scale, w.p2, w.p2_scale, _ptr(h8), _ptr(h8_scale), _ptr(y_perm),
                                       _ptr(ws), _stream()), "mohge_expert_fwd_mx8")
 
@@ -554,6 +586,9 @@ def mx8_rows(codes, scale):
 def mx8_tile_scales(scale):
     """Scale bytes [batch, rows, ceil(K / 32)] in the tiled layout of the operands."""
     B, R, n = scale.shape
+    if scale.element_size() == 1:
+        scale = scale.view(torch.uint8)         # torch.float8_e8m0fnu among them: its bytes, not its values
+    _require(not scale.is_floating_point(), "mx8_tile_scales: scales are bytes, not %s", scale.dtype)
     rb, kb = (R + 127) // 128, (n + 3) // 4
     full = torch.zeros(B, rb * 128, kb * 4, dtype=torch.uint8, device=scale.device)
     full[:, :R, :n] = scale
@@ -565,10 +600,11 @@ class Mx8Weights:
     [N, d, W_g] (E4M3) with one scale byte per 32 columns [.., ceil(K / 32)]."""
 
     def __init__(self, cfg: Config, w13, w13_scale, w2, w2_scale):
-        N, d = cfg.experts_per_group, cfg.d_model
+        N, blocks = cfg.experts_per_group, lambda k: -(-k // 32)
+        _require_weights(cfg, "Mx8Weights: codes", w13, w2, dtype=1)
+        _require_weights(cfg, "Mx8Weights: scales", w13_scale, w2_scale, blocks, blocks)
 
-        def elements(q, shape):
-            assert tuple(q.shape) == shape, "%s, expected %s" % (tuple(q.shape), shape)
+        def elements(q):
             q = q.view(torch.uint8)
             K, pitch = q.shape[2], mohge_mx8_pitch(q.shape[2])
             if pitch == K:
@@ -577,10 +613,10 @@ class Mx8Weights:
             out[:, :, :K] = q
             return out
 
-        W = list(cfg.group_width)
-        self._set([elements(q, (N, 2 * w, d)) for q, w in zip(w13, W)],
-                  [mx8_tile_scales(s.reshape(2 * N, w, -1)) for s, w in zip(w13_scale, W)],
-                  [elements(q, (N, d, w)) for q, w in zip(w2, W)], [mx8_tile_scales(s) for s in w2_scale])
+        self.layer = cfg.c().layer
+        self._set([elements(q) for q in w13],
+                  [mx8_tile_scales(s.reshape(2 * N, s.shape[1] // 2, s.shape[2])) for s in w13_scale],
+                  [elements(q) for q in w2], [mx8_tile_scales(s) for s in w2_scale])
 
     def _set(self, w13, w13_scale, w2, w2_scale):
         self.w13, self.w13_scale, self.w2, self.w2_scale = w13, w13_scale, w2, w2_scale
@@ -590,10 +626,12 @@ class Mx8Weights:
     @classmethod
     def quantize(cls, cfg: Config, w13, w2):
         """From the layer's own weights w13[g] [N, 2 W_g, d] and w2[g] [N, d, W_g]."""
+        _require_weights(cfg, "Mx8Weights.quantize", w13, w2)
         N, d = cfg.experts_per_group, cfg.d_model
         a = [quantize_mx8(w.reshape(2 * N, w.shape[1] // 2, d)) for w in w13]
         b = [quantize_mx8(w) for w in w2]
         self = cls.__new__(cls)
+        self.layer = cfg.c().layer
         self._set([x[0] for x in a], [x[1] for x in a], [x[0] for x in b], [x[1] for x in b])
         return self
 

@@ -31,3 +31,65 @@ def test_quantizing_refuses_outputs_that_are_too_small():
     for q, s, text in ((u8(2, 16, 63), u8(n), "q holds"), (u8(2, 16, 64), u8(n - 1), "scale_tiled holds")):
         with pytest.raises(B.MohgeError, match=text):
             B.mohge_quantize_mx8(w, q, s)
+
+
+CFG = dict(d_model=64, n_groups=2, experts_per_group=3, k_groups=1, k_experts=2)
+
+
+def weights(widths=(16, 32), N=3, d=64, dtype=torch.bfloat16, k=lambda n: n):
+    z = lambda *s: torch.zeros(*s).to(dtype)  # noqa: E731
+    return [z(N, 2 * w, k(d)) for w in widths], [z(N, d, k(w)) for w in widths]
+
+
+@pytest.mark.parametrize("wrong,text", [
+    (dict(widths=(16, 32, 8)), "3 w13 for 2 groups"), (dict(widths=(16,)), "1 w13 for 2 groups"),
+    (dict(widths=(32, 16)), r"w13\[0\] is"), (dict(N=2), r"w13\[0\] is"), (dict(d=72), r"w13\[0\] is")])
+def test_weights_of_another_layer_are_refused(wrong, text):
+    """Surplus and missing groups, other widths, counts or columns: the library would read past their end."""
+    cfg = B.Config(**CFG, group_width=[16, 32])
+    w13, w2 = weights(**wrong)
+    for make in (lambda: B.Mx8Weights.quantize(cfg, w13, w2), lambda: B.W4Weights.quantize(cfg, 32, w13, w2)):
+        with pytest.raises(B.MohgeError, match=text):
+            make()
+    codes = weights(**wrong, dtype=torch.uint8)
+    blocks = lambda n: -(-n // 32)  # noqa: E731
+    with pytest.raises(B.MohgeError, match=text):
+        B.Mx8Weights(cfg, codes[0], weights(**wrong, dtype=torch.uint8, k=blocks)[0], codes[1], weights(**wrong, dtype=torch.uint8, k=blocks)[1])
+    q13, q2 = weights(**wrong, dtype=torch.uint8, k=lambda n: n // 2)
+    s13, s2 = weights(**wrong, k=blocks)
+    with pytest.raises(B.MohgeError, match=text):
+        B.W4Weights(cfg, 32, q13, s13, q2, s2)
+
+
+def test_codes_and_scales_of_another_form_are_refused():
+    cfg = B.Config(**CFG, group_width=[16, 32])
+    blocks = lambda n: -(-n // 32)  # noqa: E731
+    c13, c2 = weights(dtype=torch.uint8)
+    s13, s2 = weights(dtype=torch.uint8, k=blocks)
+    with pytest.raises(B.MohgeError, match=r"codes: w13\[0\] is torch.bfloat16"):
+        B.Mx8Weights(cfg, weights()[0], s13, c2, s2)
+    with pytest.raises(B.MohgeError, match=r"scales: w2\[1\] is"):
+        B.Mx8Weights(cfg, c13, s13, c2, [s2[0], s2[1][:, :32]])          # tiles would be read past their end
+    with pytest.raises(B.MohgeError, match="scales are bytes"):
+        B.mx8_tile_scales(torch.ones(1, 4, 2))
+    one = B.mx8_tile_scales(torch.full((1, 4, 2), 130, dtype=torch.uint8).view(torch.float8_e8m0fnu))
+    assert torch.equal(one, B.mx8_tile_scales(torch.full((1, 4, 2), 130)))
+    q13, q2 = weights(dtype=torch.uint8, k=lambda n: n // 2)
+    p13, p2 = weights(k=blocks)
+    with pytest.raises(B.MohgeError, match=r"scales: w13\[0\] is torch.float32"):
+        B.W4Weights(cfg, 32, q13, [s.float() for s in p13], q2, p2)
+    with pytest.raises(B.MohgeError, match=r"codes: w2\[0\] is"):
+        B.W4Weights(cfg, 32, q13, p13, [q[:, :, :4] for q in q2], p2)
+
+
+def test_weights_are_refused_with_the_config_of_another_layer():
+    cfg = B.Config(**CFG, group_width=[16, 32])
+    w = B.Mx8Weights.__new__(B.Mx8Weights)
+    w.layer = cfg.c().layer
+    for other in (B.Config(**{**CFG, "n_groups": 3}, group_width=[16, 32, 8]), B.Config(**CFG, group_width=[16, 40])):
+        with pytest.raises(B.MohgeError, match="weights of a layer"):
+            B.mohge_expert_fwd_mx8(other, 1, None, None, None, None, w, None, None, None, None)
+        with pytest.raises(B.MohgeError, match="weights of a layer"):
+            B.mohge_expert_fwd_w4(other, 1, None, None, None, w, None, None, None)
+    same = B.Config(**{**CFG, "k_experts": 1}, group_width=(16, 32))
+    assert B._layer_of(same, w) is same.c()
