@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import operator
 import os
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
@@ -172,20 +173,22 @@ class Config:
 
     def c(self) -> mohge_config:
         """The POD of the C ABI; rebuilt only when a field has changed since the last call."""
+        # any sequence of whole numbers (list, tuple, range, array, tensor), which may be changed in place
+        widths = [operator.index(w) for w in self.group_width]
         cached = self.__dict__.get("_c_cache")
-        if cached is not None and cached[0] == self.group_width:     # a list may be changed in place
+        if cached is not None and cached[0] == widths:
             return cached[1]
         s = mohge_config()
         s.d_model, s.n_groups, s.experts_per_group = self.d_model, self.n_groups, self.experts_per_group
         s.k_groups, s.k_experts = self.k_groups, self.k_experts
         for g in range(MAX_GROUPS):
-            s.group_width[g] = self.group_width[g] if g < len(self.group_width) else 0
+            s.group_width[g] = widths[g] if g < len(widths) else 0
         s.dtype = BF16 if self.dtype == "bf16" else F32
         s.alpha_g, s.alpha_e, s.eps = self.alpha_g, self.alpha_e, self.eps
         s.f_norm_by_T, s.fe_mode, s.row_align = self.f_norm_by_T, self.fe_mode, self.row_align
         # what weights laid out for a layer depend on
         s.layer = (self.d_model, self.n_groups, self.experts_per_group, tuple(s.group_width[:self.n_groups]))
-        self.__dict__["_c_cache"] = (type(self.group_width)(self.group_width), s)
+        self.__dict__["_c_cache"] = (widths, s)
         return s
 
     @property
