@@ -534,6 +534,14 @@ class W4Weights:
         a, b = [quantize_w4(w, group_size) for w in w13], [quantize_w4(w, group_size) for w in w2]
         return cls(cfg, group_size, [x[0] for x in a], [x[1] for x in a], [x[0] for x in b], [x[1] for x in b])
 
+    def requantize(self, cfg: Config, w13, w2) -> None:
+        """The same from weights that have changed, in the memory that is there (graphs hold its addresses)."""
+        _layer_of(cfg, self)
+        _require_weights(cfg, "W4Weights.requantize", w13, w2)
+        for ws, packed, gate_up in ((w13, self.w13, True), (w2, self.w2, False)):
+            for w, out in zip(ws, packed):
+                mohge_pack_w4(*quantize_w4(w, self.group_size), self.group_size, gate_up, out)
+
 
 def w4_scratch(cfg: Config, T: int, device="cuda") -> torch.Tensor:
     n = lib().mohge_w4_scratch_bytes(C.byref(cfg.c()), T)
@@ -637,6 +645,15 @@ class Mx8Weights:
         self.layer = cfg.c().layer
         self._set([x[0] for x in a], [x[1] for x in a], [x[0] for x in b], [x[1] for x in b])
         return self
+
+    def requantize(self, cfg: Config, w13, w2) -> None:
+        """The same from weights that have changed, in the memory that is there (graphs hold its addresses)."""
+        _layer_of(cfg, self)
+        _require_weights(cfg, "Mx8Weights.requantize", w13, w2)
+        for w, q, s in zip(w13, self.w13, self.w13_scale):
+            mohge_quantize_mx8(w.reshape(-1, w.shape[1] // 2, w.shape[2]), q, s)
+        for w, q, s in zip(w2, self.w2, self.w2_scale):
+            mohge_quantize_mx8(w, q, s)
 
 
 class Mx8Buffers:

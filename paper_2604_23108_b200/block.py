@@ -18,27 +18,74 @@ from . import binding as B
 from .inputs import WORKLOADS, make_device_inputs
 
 
+class _LowBit:
+    """The experts' weights in a low-bit form, and which values of the 16-bit weights it was made from."""
+
+    def __init__(self):
+        self.form = self._seen = None
+
+    @staticmethod
+    def _version(t):
+        return None if t.is_inference() else t._version      # inference tensors count no writes
+
+    def stale(self, tensors):
+        # the aliases keep their storage alive: the same address is the same storage
+        return self._seen is None or len(self._seen) != len(tensors) or any(
+            a.data_ptr() != t.data_ptr() or v != self._version(t) for (a, v), t in zip(self._seen, tensors))
+
+    def made_from(self, tensors):
+        self._seen = [(t.detach(), self._version(t)) for t in tensors]
+
+    def forget(self):
+        self._seen = None
+
+
 class MoeBlock:
     """norm_weight [d], w_router [N_g + N_e, d], w13[g] [N, 2 W_g, d], w2[g] [N, d, W_g], all BF16 on the device.
-    Every method returns (y, h): the block's output and the residual stream that the next block adds to."""
+    Every method returns (y, h): the block's output and the residual stream that the next block adds to.
+
+    The low-bit forms of w13 and w2 are made when they are first needed and made anew, in place, after the weights have
+    changed: after a train_backward, whose step will change them, after a write that torch has counted, when another
+    tensor took their place or w4_group changed.  A write that torch does not count (through .data or a raw pointer, into
+    an inference tensor), made since the last train_backward and the last low-bit call, has to be followed by
+    requantize().  A CUDA graph reads the forms that were there when it was captured; if they are out of date at that
+    point, it makes its own at every replay."""
 
     def __init__(self, cfg: B.Config, norm_weight, w_router, w13, w2, norm_eps: float = 1e-6, w4_group: int = 128):
         self.cfg, self.eps, self.w4_group = cfg, norm_eps, w4_group
         self.norm_weight, self.w_router, self.w13, self.w2 = norm_weight, w_router, w13, w2
-        self._mx8 = self._w4 = None          # low-bit weights, made when first asked for
+        self._mx8, self._w4 = _LowBit(), _LowBit()
         self._bufs = {}
+
+    def _low_bit(self, kept, fits, make):
+        """The form in `kept`, made anew if the weights are not those it was made from."""
+        tensors = [*self.w13, *self.w2]
+        if fits(kept.form) and not kept.stale(tensors):
+            return kept.form
+        if torch.cuda.is_current_stream_capturing():
+            return make()                        # part of the graph: nothing ran that a later call could use
+        if fits(kept.form):
+            torch.cuda.synchronize(self.norm_weight.device)      # other streams may still be reading it
+            kept.form.requantize(self.cfg, self.w13, self.w2)
+        else:
+            kept.form = make()
+        torch.cuda.current_stream().synchronize()                # any stream may use it from here on
+        kept.made_from(tensors)
+        return kept.form
 
     @property
     def mx8_weights(self):
-        if self._mx8 is None:
-            self._mx8 = B.Mx8Weights.quantize(self.cfg, self.w13, self.w2)
-        return self._mx8
+        return self._low_bit(self._mx8, lambda f: f is not None, lambda: B.Mx8Weights.quantize(self.cfg, self.w13, self.w2))
 
     @property
     def w4_weights(self):
-        if self._w4 is None:
-            self._w4 = B.W4Weights.quantize(self.cfg, self.w4_group, self.w13, self.w2)
-        return self._w4
+        return self._low_bit(self._w4, lambda f: f is not None and f.group_size == self.w4_group,
+                             lambda: B.W4Weights.quantize(self.cfg, self.w4_group, self.w13, self.w2))
+
+    def requantize(self):
+        """The weights have changed: the next low-bit call makes their low-bit forms anew."""
+        self._mx8.forget()
+        self._w4.forget()
 
     def _buffers(self, kind, T):
         """Device buffers of one way of running and one batch size, allocated once."""
@@ -84,6 +131,7 @@ class MoeBlock:
         reaches h on the residual stream.  Weight gradients: grads()."""
         T = dy.shape[0]
         b = self._buffers("train", T)
+        self.requantize()                        # what follows a gradient is an update
         B.layer_backward(self.cfg, b["layer"], b["u"], self.w_router, self.w13, self.w2, dy)
         B.mohge_norm_bwd(self.cfg, T, b["layer"].dx, dh, b["h"], self.norm_weight, b["rstd"], b["dx"], b["dnorm"], False, b["ws"])
         return b["dx"]
