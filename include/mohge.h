@@ -93,7 +93,8 @@ const char* mohge_last_error(void);
  * the calling process, counted on the host at launch time. */
 int64_t mohge_launch_count(void);
 
-/* Bytes of workspace needed for T tokens (0 on invalid config). */
+/* Bytes of workspace needed for T tokens (0 on invalid config).  Not always less for fewer tokens: a
+ * workspace that serves several batch sizes has the largest of their figures. */
 int64_t mohge_workspace_bytes(const mohge_config* cfg, int64_t T);
 
 /* Number of rows every permuted buffer must have: R + N_e*(row_align-1) rounded up to

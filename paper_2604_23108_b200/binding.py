@@ -675,17 +675,30 @@ class Mx8Buffers:
         mohge_workspace_init(cfg, T, self.ws)
 
 
-def layer_forward_mx8(cfg: Config, b: Mx8Buffers, x8, x8_scale, expert_idx, gate_w, weights: Mx8Weights, y_add=None):
-    """dispatch_indices -> permute_mx8 -> expert_fwd_mx8 -> combine on routed tokens; returns b.y."""
-    T = b.T
+def _batch(cfg: Config, b, T: Optional[int]) -> int:
+    """Tokens of a call on the buffers b: all that they were made for, or the first T of them."""
+    if T is None or T == b.T:
+        return b.T
+    _require(0 <= T <= b.T, "%s tokens on buffers made for %d", T, b.T)
+    _require_bytes("the workspace", b.ws, mohge_workspace_bytes(cfg, T))     # (not always less for fewer tokens)
+    return T
+
+
+def layer_forward_mx8(cfg: Config, b: Mx8Buffers, x8, x8_scale, expert_idx, gate_w, weights: Mx8Weights, y_add=None,
+                      T: Optional[int] = None, y=None):
+    """dispatch_indices -> permute_mx8 -> expert_fwd_mx8 -> combine on routed tokens; returns y, which is b.y (the
+    next call's too) where none is given.  T: fewer tokens than the buffers were made for."""
+    T = _batch(cfg, b, T)
+    if y is None:
+        y = b.y if T == b.T else b.y[:T]
     if T == 0:
-        return b.y[:0]
+        return y[:0]
     mohge_dispatch_indices(cfg, T, expert_idx, b.counts, b.offsets, b.aligned, b.row_of, b.prow_of, b.src_of,
                            b.tok_of_prow, b.ws)
     mohge_permute_mx8(cfg, T, x8, x8_scale, b.tok_of_prow, b.xp8, b.xp8_scale)
     mohge_expert_fwd_mx8(cfg, T, b.xp8, b.xp8_scale, b.counts, b.aligned, weights, b.h8, b.h8_scale, b.y_perm, b.ws)
-    mohge_combine(cfg, T, b.y_perm, b.prow_of, gate_w, b.y, y_add=y_add)
-    return b.y
+    mohge_combine(cfg, T, b.y_perm, b.prow_of, gate_w, y, y_add=y_add)
+    return y
 
 
 class LayerBuffers:
@@ -730,12 +743,13 @@ class LayerBuffers:
 
 
 def layer_forward(cfg: Config, b: LayerBuffers, x, w_router, w13, w2, logit_bias=None,
-                  logits_in=None, aux=True, shared=None, gather=False):
+                  logits_in=None, aux=True, shared=None, gather=False, T: Optional[int] = None):
     """route -> aux_stats -> dispatch -> expert_fwd (-> shared_fwd) -> combine; results stay in
     `b`.  shared = (w13_shared, w2_shared) adds the shared experts (b.shared_width wide).
     gather: no x_perm is written; the GEMMs gather the rows of x (mohge_dispatch_indices,
-    mohge_expert_fwd_gather)."""
-    T = b.T
+    mohge_expert_fwd_gather).
+    T: fewer tokens than the buffers were made for (the first T rows of them are used)."""
+    T = _batch(cfg, b, T)
     mohge_route(cfg, T, x, w_router, logit_bias, logits_in, b.logits, b.group_idx, b.expert_idx,
                 b.gate_w, b.gs, b.esp, b.ws)
     if aux:
@@ -758,12 +772,13 @@ def layer_forward(cfg: Config, b: LayerBuffers, x, w_router, w13, w2, logit_bias
 
 
 def layer_backward(cfg: Config, b: LayerBuffers, x, w_router, w13, w2, dy, aux=True, accumulate=False,
-                   shared=None, fused_dgate=True, gather=False, dy_fused=False):
+                   shared=None, fused_dgate=True, gather=False, dy_fused=False, T: Optional[int] = None):
     """combine_bwd -> expert_bwd (-> shared_bwd) -> dispatch_bwd -> route_bwd; results stay in `b`.
     fused_dgate: the gate gradient comes out of the experts' backward (mohge_expert_bwd_dgate) and
     combine_bwd does not read y_perm; otherwise combine_bwd computes it from y_perm.
-    dy_fused: no combine_bwd and no dy_perm at all (mohge_expert_bwd_dy gathers the rows of dy)."""
-    T = b.T
+    dy_fused: no combine_bwd and no dy_perm at all (mohge_expert_bwd_dy gathers the rows of dy).
+    T: as layer_forward was given it."""
+    T = _batch(cfg, b, T)
     assert not (gather and dy_fused), "the backward without dy_perm reads x_perm: not with gather=True"
     if dy_fused:    # after a forward through x_perm
         if getattr(b, "hs", None) is None:

@@ -22,27 +22,68 @@ class _LowBit:
     """The experts' weights in a low-bit form, and which values of the 16-bit weights it was made from."""
 
     def __init__(self):
-        self.form = self._seen = None
+        self.form = self._values = self._alive = None
 
     @staticmethod
-    def _version(t):
-        return None if t.is_inference() else t._version      # inference tensors count no writes
+    def _values_of(tensors):
+        """Where the values lie, and how often torch has counted a write to them (inference tensors count none)."""
+        try:
+            return [(t.data_ptr(), t._version) for t in tensors]
+        except RuntimeError:
+            return [(t.data_ptr(), None if t.is_inference() else t._version) for t in tensors]
 
     def stale(self, tensors):
-        # the aliases keep their storage alive: the same address is the same storage
-        return self._seen is None or len(self._seen) != len(tensors) or any(
-            a.data_ptr() != t.data_ptr() or v != self._version(t) for (a, v), t in zip(self._seen, tensors))
+        return self._values != self._values_of(tensors)
 
     def made_from(self, tensors):
-        self._seen = [(t.detach(), self._version(t)) for t in tensors]
+        self._values = self._values_of(tensors)
+        self._alive = [t.detach() for t in tensors]          # their storage too: the same address is the same storage
 
     def forget(self):
-        self._seen = None
+        self._values = None
+
+
+class TrainState:
+    """What a train_forward of up to `cap` tokens leaves for its train_backward, and the gradients of the weights.
+    Forward and backward may be enqueued on different streams: each waits for the state's last use."""
+
+    def __init__(self, cfg: B.Config, T: int, device):
+        n = lambda *s, dt=cfg.torch_dtype: torch.empty(*s, dtype=dt, device=device)  # noqa: E731
+        self.cap = max(1, T)
+        self.layer = B.LayerBuffers(cfg, self.cap, device)
+        self.u, self.rstd = n(self.cap, cfg.d_model), n(self.cap, dt=torch.float32)
+        self.dnorm = n(cfg.d_model, dt=torch.float32)
+        self.T = self.grads_T = self.h = self.dx = None       # tokens of the latest forward and of the latest backward
+        self._home, self._event = B._stream(), torch.cuda.Event()
+        self.leave()
+
+    def enter(self):
+        if B._stream() != self._last and not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream().wait_event(self._event)
+
+    def leave(self):
+        self._last = B._stream()
+        if torch.cuda.is_current_stream_capturing():
+            return
+        self._event.record()
+        if self._last != self._home:             # the allocator is told of a stream that it does not know uses them
+            for v in (*vars(self).values(), *vars(self.layer).values()):
+                for t in v if isinstance(v, list) else [v]:
+                    if isinstance(t, torch.Tensor):
+                        t.record_stream(torch.cuda.current_stream())
 
 
 class MoeBlock:
-    """norm_weight [d], w_router [N_g + N_e, d], w13[g] [N, 2 W_g, d], w2[g] [N, d, W_g], all BF16 on the device.
-    Every method returns (y, h): the block's output and the residual stream that the next block adds to.
+    """norm_weight [d], w_router [N_g + N_e, d], w13[g] [N, 2 W_g, d], w2[g] [N, d, W_g], all of the config's type on the
+    device (prompt and tokens: BF16).  x and residual are [T, d] of that type, T any number of tokens.  The forward
+    methods return (y, h): the block's output and the residual stream that the next block adds to.
+
+    Results are tensors of their own, which no later call writes, unless a caller gives prompt or tokens the pair to
+    write, out=(y, h), h possibly x or residual (allocating them is 3 of some 35 us of host time for a token).  h is
+    also what train_backward reads: leave it as it is until then.  Working buffers are kept, one set for each way of running and stream, as large as the largest batch
+    so far (release() frees them); inside a CUDA graph every call has buffers of its own, from the graph's memory.
+    train_backward belongs to the latest train_forward; for several forwards in flight give each a state of its own,
+    train_state(T), and hand it to both calls.
 
     The low-bit forms of w13 and w2 are made when they are first needed and made anew, in place, after the weights have
     changed: after a train_backward, whose step will change them, after a write that torch has counted, when another
@@ -55,7 +96,8 @@ class MoeBlock:
         self.cfg, self.eps, self.w4_group = cfg, norm_eps, w4_group
         self.norm_weight, self.w_router, self.w13, self.w2 = norm_weight, w_router, w13, w2
         self._mx8, self._w4 = _LowBit(), _LowBit()
-        self._bufs = {}
+        self._sets = {}                      # (way of running, stream): its buffers
+        self._train = self._train_captured = self._graded = None
 
     def _low_bit(self, kept, fits, make):
         """The form in `kept`, made anew if the weights are not those it was made from."""
@@ -64,8 +106,9 @@ class MoeBlock:
             return kept.form
         if torch.cuda.is_current_stream_capturing():
             return make()                        # part of the graph: nothing ran that a later call could use
-        if fits(kept.form):
+        if kept.form is not None:
             torch.cuda.synchronize(self.norm_weight.device)      # other streams may still be reading it
+        if fits(kept.form):
             kept.form.requantize(self.cfg, self.w13, self.w2)
         else:
             kept.form = make()
@@ -87,73 +130,166 @@ class MoeBlock:
         self._mx8.forget()
         self._w4.forget()
 
-    def _buffers(self, kind, T):
-        """Device buffers of one way of running and one batch size, allocated once."""
-        key = (kind, T)
-        if key not in self._bufs:
-            cfg, dev = self.cfg, self.norm_weight.device
-            n = lambda *s, dt=torch.bfloat16: torch.empty(*s, dtype=dt, device=dev)  # noqa: E731
-            b = {"h": n(T, cfg.d_model), "u": n(T, cfg.d_model), "rstd": n(T, dt=torch.float32)}
-            if kind == "train":
-                b["layer"] = B.LayerBuffers(cfg, T, dev)
-                b["dx"], b["dnorm"] = n(T, cfg.d_model), n(cfg.d_model, dt=torch.float32)
-                b["ws"] = b["layer"].ws
-            else:
-                f32, i32 = torch.float32, torch.int32
-                b["route"] = (n(T, cfg.n_logits, dt=f32), n(T, cfg.k_groups, dt=i32), n(T, cfg.k_experts, dt=i32),
-                              n(T, cfg.k_experts, dt=f32), n(T, cfg.n_groups, dt=f32), n(T, cfg.n_experts, dt=f32))
-                if kind == "prompt":
-                    b["experts"] = B.Mx8Buffers(cfg, T, dev)
-                    b["ws"] = b["experts"].ws
-                    b["u8"] = B.mx8_empty(T, cfg.d_model, dev)
-                else:
-                    b["ws"] = B.new_workspace(cfg, T, dev)
-                    b["scratch"], b["y"] = B.w4_scratch(cfg, T, dev), n(T, cfg.d_model)
-            self._bufs[key] = b
-        return self._bufs[key]
+    def release(self):
+        """Frees the working buffers (calls that use them have to be complete, or enqueued on the current stream)."""
+        self._sets.clear()
+        self._train = self._train_captured = self._graded = None
 
-    def _norm(self, b, T, x, residual, u8=(None, None)):
-        B.mohge_norm_fwd(self.cfg, T, x, residual, self.norm_weight, self.eps, b["h"], b["u"], u8[0], u8[1], b["rstd"])
+    def _tokens_of(self, x, other=None, names=("x", "residual")):
+        T, shape, want = x.shape[0], x.shape, self.cfg.torch_dtype
+        if len(shape) != 2 or shape[1] != self.cfg.d_model or x.dtype is not want:
+            raise B.MohgeError("%s is %s %s, expected %s [T, %d]" % (names[0], x.dtype, tuple(shape), want, self.cfg.d_model))
+        if other is not None and (other.shape != shape or other.dtype is not want):
+            raise B.MohgeError("%s is %s %s, expected %s %s" % (names[1], other.dtype, tuple(other.shape), want, tuple(shape)))
+        return T
+
+    # ---- serving
+
+    def _serving(self, kind, T):
+        """Buffers of a prompt or tokens call: the stream's set, grown if the batch is the largest so far."""
+        capturing = torch.cuda.is_current_stream_capturing()
+        key = (kind, B._stream())
+        s = None if capturing else self._sets.get(key)
+        if s is None or s["cap"] < T:
+            s = None
+            if not capturing:
+                self._sets.pop(key, None)        # freed before the larger one is made
+            cfg, dev, f32, i32 = self.cfg, self.norm_weight.device, torch.float32, torch.int32
+            n = lambda *sh, dt=torch.bfloat16: torch.empty(*sh, dtype=dt, device=dev)  # noqa: E731
+            s = {"cap": T, "T": None, "u": n(T, cfg.d_model),
+                 "route": (n(T, cfg.n_logits, dt=f32), n(T, cfg.k_groups, dt=i32), n(T, cfg.k_experts, dt=i32),
+                           n(T, cfg.k_experts, dt=f32), n(T, cfg.n_groups, dt=f32), n(T, cfg.n_experts, dt=f32))}
+            if kind == "prompt":
+                s["experts"], s["u8"] = B.Mx8Buffers(cfg, T, dev), B.mx8_empty(T, cfg.d_model, dev)
+                s["ws"] = s["experts"].ws
+            else:
+                s["ws"], s["scratch"] = B.new_workspace(cfg, T, dev), B.w4_scratch(cfg, T, dev)
+            if not capturing:
+                self._sets[key] = s
+        if s["T"] != T:
+            if B.mohge_workspace_bytes(self.cfg, T) > s["ws"].numel():    # not always less for fewer tokens
+                s["ws"] = B.new_workspace(self.cfg, T, s["ws"].device)
+                if kind == "prompt":
+                    s["experts"].ws = s["ws"]
+            b = s["view"] = {"u": s["u"][:T], "route": tuple(t[:T] for t in s["route"]), "ws": s["ws"]}
+            if kind == "prompt":
+                b["experts"], b["u8"] = s["experts"], tuple(t[:T] for t in s["u8"])
+            else:
+                b["scratch"] = s["scratch"]
+            s["T"] = T
+        return s["view"]
+
+    def _outputs(self, x, out):
+        if out is None:
+            return torch.empty_like(x), torch.empty_like(x)
+        self._tokens_of(x, out[0], ("x", "y"))
+        self._tokens_of(x, out[1], ("x", "h"))
+        return out
+
+    def _norm(self, T, x, residual, u, h, u8=(None, None), rstd=None):
+        B.mohge_norm_fwd(self.cfg, T, x, residual, self.norm_weight, self.eps, h, u, u8[0], u8[1], rstd)
 
     def _route(self, b, T):
         logits, group_idx, expert_idx, gate, gs, esp = b["route"]
         B.mohge_route(self.cfg, T, b["u"], self.w_router, None, None, logits, group_idx, expert_idx, gate, gs, esp, b["ws"])
         return expert_idx, gate
 
-    def train_forward(self, x, residual=None):
-        T = x.shape[0]
-        b = self._buffers("train", T)
-        self._norm(b, T, x, residual)
-        return B.layer_forward(self.cfg, b["layer"], b["u"], self.w_router, self.w13, self.w2), b["h"]
+    def prompt(self, x, residual=None, out=None):
+        T = self._tokens_of(x, residual)
+        y, h = self._outputs(x, out)
+        if T > 0:
+            weights = self.mx8_weights
+            b = self._serving("prompt", T)
+            self._norm(T, x, residual, b["u"], h, b["u8"])
+            expert_idx, gate = self._route(b, T)
+            B.layer_forward_mx8(self.cfg, b["experts"], *b["u8"], expert_idx, gate, weights, T=T, y=y)
+        return y, h
 
-    def train_backward(self, dy, dh=None):
-        """Gradient of x (and of the residual) after train_forward on the same batch size; dh is the gradient that
-        reaches h on the residual stream.  Weight gradients: grads()."""
-        T = dy.shape[0]
-        b = self._buffers("train", T)
+    def tokens(self, x, residual=None, out=None):
+        T = self._tokens_of(x, residual)
+        y, h = self._outputs(x, out)
+        if T > 0:
+            weights = self.w4_weights
+            b = self._serving("tokens", T)
+            self._norm(T, x, residual, b["u"], h)
+            expert_idx, gate = self._route(b, T)
+            B.mohge_expert_fwd_w4(self.cfg, T, b["u"], expert_idx, gate, weights, b["scratch"], y, b["ws"])
+        return y, h
+
+    # ---- training
+
+    def train_state(self, T):
+        """A state for forwards of up to T tokens that other forwards leave alone."""
+        return TrainState(self.cfg, T, self.norm_weight.device)
+
+    def _own_state(self, T):
+        """The block's state, for a forward of T tokens."""
+        if torch.cuda.is_current_stream_capturing():
+            self._train_captured = self.train_state(T)
+            return self._train_captured
+        st = self._train
+        if st is not None and st.cap < T:
+            st = self._train = self._graded = None                # freed before the larger one is made
+        if st is None:
+            st = self._train = self.train_state(T)
+        return st
+
+    def train_forward(self, x, residual=None, state=None):
+        T = self._tokens_of(x, residual)
+        st = state or self._own_state(T)
+        if T > st.cap:
+            raise B.MohgeError("train_forward of %d tokens with a state for %d" % (T, st.cap))
+        st.enter()
+        L = st.layer
+        st.T = None
+        L.y, st.h = self._outputs(x, None)
+        if T > 0:
+            if B.mohge_workspace_bytes(self.cfg, T) > L.ws.numel():       # not always less for fewer tokens
+                L.ws = B.new_workspace(self.cfg, T, L.ws.device)
+            self._norm(T, x, residual, st.u, st.h, rstd=st.rstd)
+            B.layer_forward(self.cfg, L, st.u, self.w_router, self.w13, self.w2, T=T)
+        st.T = T
+        st.leave()
+        return L.y, st.h
+
+    def train_backward(self, dy, dh=None, state=None):
+        """Gradient of x (and of the residual) of the latest train_forward (of the state's, where one is given); dh is
+        the gradient that reaches h on the residual stream.  Weight gradients: grads()."""
+        T = self._tokens_of(dy, dh, ("dy", "dh"))
+        st = state or (self._train_captured if torch.cuda.is_current_stream_capturing() else self._train)
+        if st is None or st.T != T:
+            raise B.MohgeError("train_backward of %d tokens: the latest train_forward of this state had %s"
+                               % (T, "none" if st is None or st.T is None else st.T))
         self.requantize()                        # what follows a gradient is an update
-        B.layer_backward(self.cfg, b["layer"], b["u"], self.w_router, self.w13, self.w2, dy)
-        B.mohge_norm_bwd(self.cfg, T, b["layer"].dx, dh, b["h"], self.norm_weight, b["rstd"], b["dx"], b["dnorm"], False, b["ws"])
-        return b["dx"]
+        st.enter()
+        L, st.dx = st.layer, torch.empty_like(dy)
+        if T == 0:
+            for g in (st.dnorm, L.dw_router, *L.dw13, *L.dw2):
+                g.zero_()
+        else:
+            B.layer_backward(self.cfg, L, st.u, self.w_router, self.w13, self.w2, dy, T=T)
+            B.mohge_norm_bwd(self.cfg, T, L.dx, dh, st.h, self.norm_weight, st.rstd, st.dx, st.dnorm, False, L.ws)
+        st.grads_T = T
+        st.leave()
+        if state is None:
+            self._graded = st
+        return st.dx
 
-    def grads(self, T):
-        b = self._buffers("train", T)
-        return {"norm": b["dnorm"], "router": b["layer"].dw_router, "w13": b["layer"].dw13, "w2": b["layer"].dw2}
+    def grads(self, T=None, state=None):
+        """The weights' gradients that the latest train_backward (of T tokens) wrote; the next one overwrites them."""
+        st = state or self._graded
+        if st is None or st.grads_T is None or T not in (None, st.grads_T):
+            raise B.MohgeError("grads: no train_backward%s" % ("" if T is None else " of %d tokens" % T))
+        return {"norm": st.dnorm, "router": st.layer.dw_router, "w13": st.layer.dw13, "w2": st.layer.dw2}
 
-    def prompt(self, x, residual=None):
-        T = x.shape[0]
-        b = self._buffers("prompt", T)
-        self._norm(b, T, x, residual, b["u8"])
-        expert_idx, gate = self._route(b, T)
-        return B.layer_forward_mx8(self.cfg, b["experts"], *b["u8"], expert_idx, gate, self.mx8_weights), b["h"]
-
-    def tokens(self, x, residual=None):
-        T = x.shape[0]
-        b = self._buffers("tokens", T)
-        self._norm(b, T, x, residual)
-        expert_idx, gate = self._route(b, T)
-        B.mohge_expert_fwd_w4(self.cfg, T, b["u"], expert_idx, gate, self.w4_weights, b["scratch"], b["y"], b["ws"])
-        return b["y"], b["h"]
+    def _buffers(self, kind, T):
+        """The working buffers of a way of running, as a call of T tokens on this stream finds them."""
+        if kind != "train":
+            return self._serving(kind, T)
+        st = self._train if self._train is not None and self._train.cap >= T else self._own_state(T)
+        if st.dx is None or st.dx.shape[0] != T:
+            st.dx = torch.empty(T, self.cfg.d_model, dtype=self.cfg.torch_dtype, device=st.u.device)
+        return {"layer": st.layer, "u": st.u[:T], "h": st.h, "rstd": st.rstd[:T], "dx": st.dx, "dnorm": st.dnorm, "ws": st.layer.ws}
 
 
 def _time(fn, calls):

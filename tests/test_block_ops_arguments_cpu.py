@@ -93,3 +93,31 @@ def test_weights_are_refused_with_the_config_of_another_layer():
             B.mohge_expert_fwd_w4(other, 1, None, None, None, w, None, None, None)
     same = B.Config(**{**CFG, "k_experts": 1}, group_width=(16, 32))
     assert B._layer_of(same, w) is same.c()
+
+
+def test_a_block_refuses_tokens_of_another_type_or_shape():
+    from paper_2604_23108_b200.block import MoeBlock
+    cfg = B.Config(**CFG, group_width=[16, 32])
+    w13, w2 = weights()
+    block = MoeBlock(cfg, torch.ones(64).bfloat16(), torch.zeros(8, 64).bfloat16(), w13, w2)
+    x = torch.zeros(3, 64).bfloat16()
+    for bad, args in (("x is torch.float32", (x.float(),)), ("x is torch.float16", (x.half(),)), (r"x is .*\(3, 56\)", (x[:, :56],)),
+                      (r"residual is .*\(2, 64\)", (x, x[:2])), ("residual is torch.float32", (x, x.float()))):
+        for call in (block.prompt, block.tokens, block.train_forward):
+            with pytest.raises(B.MohgeError, match=bad):
+                call(*args)
+    with pytest.raises(B.MohgeError, match="dh is torch.float32"):
+        block.train_backward(x, x.float())
+
+
+def test_fewer_tokens_than_the_buffers_were_made_for():
+    """The workspace is not always smaller for fewer tokens (the router backward's partial sums): checked, not assumed."""
+    from types import SimpleNamespace
+    cfg = B.Config(**{**CFG, "d_model": 1024}, group_width=[16, 32])
+    T = next(t for t in range(64, 8192, 64) if B.mohge_workspace_bytes(cfg, t) > B.mohge_workspace_bytes(cfg, t + 64))
+    b = SimpleNamespace(T=T + 64, ws=torch.empty(B.mohge_workspace_bytes(cfg, T + 64), dtype=torch.uint8))
+    assert B._batch(cfg, b, None) == B._batch(cfg, b, T + 64) == T + 64 and B._batch(cfg, b, 1) == 1
+    with pytest.raises(B.MohgeError, match="workspace"):
+        B._batch(cfg, b, T)
+    with pytest.raises(B.MohgeError, match="made for"):
+        B._batch(cfg, b, T + 65)
