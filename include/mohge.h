@@ -424,7 +424,9 @@ int64_t mohge_mx8_tiled_bytes(int64_t batch, int64_t rows, int64_t K);
  *   y [T, d] dtype, nullable           y8, y8_scale: y in the mx8 rows layout, both or neither
  *   rstd [T] float32, nullable (mohge_norm_bwd needs it)
  * At least one of y and y8.  Sums in FP32; the statistics and y come from the unrounded sum.  A row with
- * an infinity or a NaN gives NaN where the definition does and touches no other row.
+ * an infinity or a NaN gives NaN where the definition does and touches no other row.  A finite row whose
+ * sum of squares leaves FP32's range (elements above some 1.8e19 / sqrt(d_model)) has rstd = 0 and so y = 0;
+ * with norm_eps = 0 one whose squares all vanish in FP32 has an infinite rstd.
  * d_model <= 16384 (a row is kept in the registers of one block).
  */
 int32_t mohge_norm_fwd(const mohge_config* cfg, int64_t T, const void* x, const void* residual,
@@ -437,7 +439,8 @@ int32_t mohge_norm_fwd(const mohge_config* cfg, int64_t T, const void* x, const 
  *   dh [T, d] dtype, nullable: gradient that reaches h on the residual stream.  dx is the gradient of x
  *   and of the residual alike; it may be dy or dh itself.
  *   dweight [d] float32; accumulate != 0 adds into it.  Partial sums per CTA go through ws and are added
- *   in a fixed order: the same inputs give the same bits.
+ *   in a fixed order: the same inputs give the same bits.  A row with rstd = 0 has dx = dh (or 0) and
+ *   adds nothing to dweight.
  */
 int32_t mohge_norm_bwd(const mohge_config* cfg, int64_t T, const void* dy, const void* dh, const void* h,
                        const void* weight, const float* rstd, void* dx, float* dweight,

@@ -264,9 +264,10 @@ norm_bwd_kernel(int64_t T_rows, int d, int stages, const T* dy, const T* dh, con
         pw[i].get(w);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float2 ab = __fmul2_rn(a[j], b[j]);
-          dot2 = __ffma2_rn(ab, w[j], dot2);
-          dw[i][j] = __ffma2_rn(ab, two(rs), dw[i][j]);
+          // xhat before its product with dy: h dy leaves FP32's range first, and one such row would be in all of dweight
+          const float2 ax = __fmul2_rn(a[j], __fmul2_rn(b[j], two(rs)));
+          dot2 = __ffma2_rn(ax, w[j], dot2);
+          dw[i][j] = __fadd2_rn(dw[i][j], ax);
         }
       }
     }
@@ -279,8 +280,8 @@ norm_bwd_kernel(int64_t T_rows, int d, int stages, const T* dy, const T* dh, con
 #pragma unroll
       for (int w = 0; w < TPR / 32; ++w) dot += slots[g][turn][w];
     }
-    // dx = rs a w - (rs mean(g xhat) rs) b + dh, the last two first
-    const float2 c = two(-(dot * rs / (float)d) * rs * rs), rs2 = two(rs);
+    // dx = rs (a w - (rs mean(g xhat)) b) + dh: without rs^2, which has half of rs's range
+    const float2 c = two(-(dot / (float)d) * rs), rs2 = two(rs);
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
       const int p = i * TPR + t;
@@ -297,8 +298,10 @@ norm_bwd_kernel(int64_t T_rows, int d, int stages, const T* dy, const T* dh, con
           q.get(e);
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          a[j] = __ffma2_rn(__fmul2_rn(a[j], w[j]), rs2, dh ? __ffma2_rn(b[j], c, e[j]) : __fmul2_rn(b[j], c));
+        for (int j = 0; j < 4; ++j) {
+          const float2 g = __ffma2_rn(b[j], c, __fmul2_rn(a[j], w[j]));
+          a[j] = dh ? __ffma2_rn(g, rs2, e[j]) : __fmul2_rn(g, rs2);
+        }
         q.set(a);
         q.store(dx + row * d + 8 * p);
       }
