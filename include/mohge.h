@@ -109,7 +109,7 @@ int32_t mohge_workspace_init(const mohge_config* cfg, int64_t T, void* ws, int64
 /* Copies the device status word to *host_out (HOST) and synchronises `stream`; the only
  * device-to-host transfer in the library, off the hot path.  The word is 0 when nothing was
  * reported, else (code << 24) | detail, first report wins:
- *   code 1  a bounded wait in the grouped GEMM kernel expired   -> returns MOHGE_ERR_TIMEOUT
+ *   code 1  a bounded wait in a kernel (the message says which) expired -> returns MOHGE_ERR_TIMEOUT
  *   code 2  an index check failed and the entry was skipped     -> returns MOHGE_ERR_DEVICE_CHECK
  *   code 3  NaN among the router logits (read as the most negative float, i.e. ranked below
  *           every number: Eq. 2-5 order real numbers and define nothing for NaN)

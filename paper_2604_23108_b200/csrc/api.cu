@@ -277,7 +277,10 @@ int32_t mohge_get_device_status(const void* ws, int32_t* host_out, void* stream)
   const int32_t word = *host_out, code = word >> 24, site = word & 0xffffff;
   if (word == 0) return MOHGE_OK;
   if (code == 1) {
-    set_error("a device-side wait gave up after its time budget (site %d of the grouped GEMM kernel)", site);
+    // sites are numbered per kernel: 1..8 gemm_tc.cu, 21..25 gemm_mx8.cu, 41 experts_w4.cu, 51 norm.cu
+    set_error("a device-side wait gave up after its time budget (site %d of %s)", site,
+              site < 20 ? "the grouped GEMM kernel" : site < 40 ? "the 8-bit experts" : site < 50 ? "the 4-bit experts"
+                                                                                                    : "the norm's backward");
     return MOHGE_ERR_TIMEOUT;
   }
   set_error(code == 2 ? "a device-side index check failed (site %d): the entry was skipped"
