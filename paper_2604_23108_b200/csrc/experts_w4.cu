@@ -24,19 +24,24 @@
 //     the FP32 sum of the group, so no rounding is spent on the weights.
 //   - Tokens therefore enter as FP16 too, each scaled by the power of two that takes its largest element
 //     to 2^14..2^15: the BF16 elements of x are exact down to 2^-29 of the largest (and within 2^-39 of it
-//     below), the hidden activations, kept in FP32 between the two products, get 11 significant bits.
+//     below), the hidden activations, kept in FP32 between the two products, get 11 significant bits.  One
+//     operand, because two parts (16 bits) double the second product's matrix instructions and its tokens'
+//     shared memory; an activation is off by at most 2^-12 of itself for it, and the output's error against
+//     64 bits is 0.0016-0.0017 of its size, that of rounding y to BF16 (a plain form that keeps the
+//     activations in 32 bits has the same two digits).
 //   - Work is cut evenly over the SMs by cost: the chunks (expert, up to 8 of its tokens) lie on one
 //     line, chunk after chunk, tile row after tile row, and every CTA takes an equal stretch of it (whole
 //     tile rows).  Ahead of a chunk's rows the line has what beginning the chunk costs (chunk_cost; one
-//     token through the large layer 28.3 -> 20-25 us, seven through the 1024-wide one 23.1 -> 18.4, 64
-//     242 -> 236).  Inside a CTA the 16 warps cut the stretch again into equal runs of tiles, wherever in
-//     a row that falls.  A run is contiguous in memory: one lane brings it with untiled bulk copies, four
-//     tiles each, into a ring of the warp's own in shared memory, as deep as the tokens leave room (two
+//     token through the large layer 28.3 -> 20-25 us in calls that repeat, so that its weights are in L2
+//     (26-27 from DRAM now), seven through the 1024-wide one 23.1 -> 18.4, 64 242 -> 236).
+//     Inside a CTA the 16 warps cut the stretch again into equal runs of tiles, wherever in a row that
+//     falls.  A run is contiguous in memory: one lane brings it with untiled bulk copies, four tiles
+//     each, into a ring of the warp's own in shared memory, as deep as the tokens leave room (two
 //     copies, 130 KB in flight per SM, at eight tokens and d = 4096).  (Loads into registers, six tiles
 //     ahead, reached 3.2 TB/s: the hardware tracks too few of them apart.)  A row that lies inside a run
 //     is finished by its warp alone, and rows that runs share are added up in warp order after one barrier
 //     per chunk.  Nothing depends on timing: the same inputs give the same bits.
-//   - At 64 tokens the call takes 230-236 us for 1.05 GB (4.5 TB/s): the integer pipe is busy half of the
+//   - At 64 tokens the call takes 233-238 us for 1.05 GB (4.4 TB/s): the integer pipe is busy half of the
 //     time and nothing is streamed while a chunk's tokens are staged.
 // The second product's results are kept per (token, expert) pair in FP32 and added over a token's
 // experts, in slot order, by combine_w4_kernel, which rounds once.
