@@ -228,3 +228,20 @@ def test_no_tokens():
     block.train_forward(x)
     block.train_backward(x)
     assert not any(t.any() for t in grads(block))
+
+
+def test_a_training_step_of_an_fp32_layer():
+    """Buffers of the config's type.  FP32 against the same step in BF16 on values that BF16 holds exactly."""
+    block, _ = make()
+    c = block.cfg
+    cfg = B.Config(c.d_model, c.n_groups, c.experts_per_group, c.k_groups, c.k_experts, list(c.group_width), dtype="f32", row_align=1)
+    wide = MoeBlock(cfg, block.norm_weight.float(), block.w_router.float(), [w.float() for w in block.w13], [w.float() for w in block.w2])
+    a = [normal(i, 50) for i in range(4)]
+    low, high = step(block, *a), step(wide, *[t.float() for t in a])
+    assert all(t.dtype == torch.float32 for t in high[:3])
+    routed = (block._train.layer.expert_idx == wide._train.layer.expert_idx).all(dim=1)
+    assert routed.float().mean() > 0.9                       # BF16's rounding of the norm's output moves few tokens
+    for u, v in zip(low[:3], high[:3]):
+        assert float((u.float() - v)[routed].norm() / v[routed].norm()) <= 2e-2
+    with pytest.raises(B.MohgeError, match="BF16"):
+        wide.tokens(a[0].float())
