@@ -476,7 +476,8 @@ int32_t mohge_pack_w4(int64_t batch, int64_t rows, int32_t K, int32_t group_size
  *   y_add [T, d] BF16, nullable; y [T, d] BF16
  *   scratch: mohge_w4_scratch_bytes(cfg, T) bytes, 16-byte aligned, contents immaterial
  * FP32 sums; the hidden activations enter the second product with 11 significant bits (FP16, scaled by a
- * power of two per token and expert), y is rounded once.  An expert that occurs
+ * power of two per token and expert), x exactly down to 2^-29 of the token's largest element and within 2^-39 of
+ * that below, y is rounded once.  An expert that occurs
  * twice for a token counts twice; an index outside 0..N_e-1 contributes nothing and is reported in the
  * status word (code 2).  Any T: batches beyond 64 tokens (or 512 / K_e) run as passes of that many, each
  * streaming the weights of the experts it hits, so prompts are better served by mohge_expert_fwd or

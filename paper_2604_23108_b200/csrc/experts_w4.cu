@@ -33,7 +33,7 @@
 //     line, chunk after chunk, tile row after tile row, and every CTA takes an equal stretch of it (whole
 //     tile rows).  Ahead of a chunk's rows the line has what beginning the chunk costs (chunk_cost; one
 //     token through the large layer 28.3 -> 20-25 us in calls that repeat, so that its weights are in L2
-//     (26-27 from DRAM now), seven through the 1024-wide one 23.1 -> 18.4, 64 242 -> 236).
+//     (24-27 from DRAM now), seven through the 1024-wide one 23.1 -> 18.4, 64 242 -> 236).
 //     Inside a CTA the 16 warps cut the stretch again into equal runs of tiles, wherever in a row that
 //     falls.  A run is contiguous in memory: one lane brings it with untiled bulk copies, four tiles
 //     each, into a ring of the warp's own in shared memory, as deep as the tokens leave room (two

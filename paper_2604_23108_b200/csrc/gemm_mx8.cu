@@ -27,7 +27,7 @@
 //
 // What it reaches: 65536 tokens of the large layer (dispatch to combine) 7.9 ms for one call on an idle GPU and
 // 9.1-9.6 ms in calls that follow each other, where the power cap holds the SM clock at 1.1 GHz of 1.965 (the first
-// product's loop takes 555 clocks per 128 columns, the instructions 512); 256 tokens 376-386 us, 81 % of the
+// product's loop takes 555 clocks per 128 columns, the instructions 512); 256 tokens 376-391 us, 81 % of the
 // DRAM's peak in the first product.  Where the contraction is short (d = 1024: eight steps) the 1300 or so
 // clocks between tiles count; eight epilogue warps or a list read further ahead did not shorten them.
 //
